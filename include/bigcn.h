@@ -426,9 +426,11 @@ bigcn_status bigcn_layernorm(const void* x, bigcn_dtype xtype, int64_t rows, int
  *           it overlaps no other argument.
  *   dgamma, dbeta  fp32[cols]; with rows == 0 they are set to zero.
  *   workspace  bigcn_layernorm_backward_workspace_bytes(rows, cols) bytes, 256-byte
- *           aligned, contents on entry ignored; needed for dgamma or dbeta only.
- * Sums over rows are formed over fixed sets of rows, short runs in fp32 and
- * those in fp64, in a fixed order: results are reproducible bit for bit.
+ *           aligned, contents on entry ignored; needed for dgamma or dbeta only.  At most
+ *           8 KB a column up to 1536 columns, about rows * cols / 8 bytes above.
+ * Sums over rows are formed over fixed sets of rows, runs of at most 69 additions in
+ * fp32 and those in fp64 (a set's sum is rounded to fp32 once before the sets are
+ * added), in a fixed order: results are reproducible bit for bit.
  * Errors: EINVAL (as bigcn_layernorm; x and codes both given or neither), EALIGN,
  *         EWORKSPACE, EUNSUPPORTED (cols > 8192 or rows >= 2^31).
  * ------------------------------------------------------------------------- */

@@ -210,9 +210,11 @@ struct Kept {
 // fp32: 45-49 and 37; 232965 x 602 bf16: 158 and 135 (5.3).
 // Each row is held in registers as in the forward, blocks taking rows in
 // turn; dx is written, and each lane adds its columns' terms of dgamma and dbeta over
-// the rows it sees in fp32, in runs of kRun turns.  A wave's runs are added up in LDS
-// and a block's waves joined at its end: part[block][2][cols]; where a row takes a
-// block every run leaves a part of its own, part[run][block].
+// the rows it sees in fp32, in runs of kRun turns, at whose end the block's lanes and
+// waves are joined: a chain of at most 69 additions of fp32.  A block's runs are added up
+// in fp64 in LDS and leave one part, rounded once: part[block][2][cols].  Where a row
+// takes a block every run leaves a part of its own, part[run][block].  (Runs added to
+// fp64 sums in memory instead cost 1-4 %: 300000 x 2048 bf16 721 -> 748 us.)
 constexpr int kRun = 64;
 
 template <typename T, bool Q8, int W, int L, int NV, bool TINY>
@@ -225,6 +227,7 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm_grad(
   constexpr int kRB = W > 1 ? 1 : kW * Map::kRows;
   __shared__ float slots[2][2][W];
   __shared__ float red[W > 1 ? 1 : 2 * kW][W > 1 ? 1 : NV * Map::kStep];
+  __shared__ double sums[2][W > 1 ? 1 : NV * Map::kStep];  // (column c: thread c mod kB alone)
   const Map m(cols);
   const int sub = W > 1 ? 0 : (int)(threadIdx.x / L);
   const int l16 = m.t & 15, group16 = l16 * (Map::kLanes / 16) + (m.t >> 4);
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm_grad(
   const int64_t stride = (int64_t)gridDim.x * kRB;
   const int wave = threadIdx.x >> 6;
   int64_t i0 = (int64_t)blockIdx.x * kRB;
-  for (int64_t at = blockIdx.x; i0 < rows; at += gridDim.x) {
+  for (int64_t run = 0; i0 < rows; ++run) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) dg[v] = db[v] = f32x4{0.f, 0.f, 0.f, 0.f};
     int32_t n = 0;
@@ -358,7 +361,7 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm_grad(
     }
     if (part == nullptr) continue;
     if constexpr (W > 1) {
-      float* pg = part + at * 2 * cols;
+      float* pg = part + (run * gridDim.x + blockIdx.x) * 2 * cols;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         m.template store<F32>(pg + 4 * m.t, k, dg[k]);
@@ -367,6 +370,7 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm_grad(
     } else {
       // The wave's rows together, then chunk k of lane t at LDS column 4 (k L + t),
       // whatever row columns it is (those a lane holds for another are zero).
+      if (run > 0) __syncthreads();
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
 #pragma unroll
@@ -384,38 +388,41 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm_grad(
           db[k][u] = b;
         }
         if ((threadIdx.x & 63) < L) {
-          f32x4* rg = reinterpret_cast<f32x4*>(&red[wave][k * Map::kStep + 4 * m.t]);
-          f32x4* rb = reinterpret_cast<f32x4*>(&red[kW + wave][k * Map::kStep + 4 * m.t]);
-          *rg = at == blockIdx.x ? dg[k] : *rg + dg[k];
-          *rb = at == blockIdx.x ? db[k] : *rb + db[k];
+          *reinterpret_cast<f32x4*>(&red[wave][k * Map::kStep + 4 * m.t]) = dg[k];
+          *reinterpret_cast<f32x4*>(&red[kW + wave][k * Map::kStep + 4 * m.t]) = db[k];
         }
       }
-    }
-  }
-  if constexpr (W == 1) {
-    if (part == nullptr) return;
-    float* pg = part + (int64_t)blockIdx.x * 2 * cols;
-    __syncthreads();
-    for (int c = threadIdx.x; c < cols; c += kB) {
-      // a lane that took the row's last four columns holds column c `back` places on
-      const int back = !TINY && c >= (NV - 1) * Map::kStep && (c & ~3) + 4 > cols
-                           ? 4 - (cols & 3) : 0;
-      float g = 0.f, b = 0.f;
+      __syncthreads();
+      float* pg = part + (int64_t)blockIdx.x * 2 * cols;
+      for (int c = threadIdx.x; c < cols; c += kB) {
+        // a lane that took the row's last four columns holds column c `back` places on
+        const int back = !TINY && c >= (NV - 1) * Map::kStep && (c & ~3) + 4 > cols
+                             ? 4 - (cols & 3) : 0;
+        float g = 0.f, b = 0.f;
 #pragma unroll
-      for (int w = 0; w < kW; ++w) {
-        g += red[w][c + back];
-        b += red[kW + w][c + back];
+        for (int w = 0; w < kW; ++w) {
+          g += red[w][c + back];
+          b += red[kW + w][c + back];
+        }
+        const double g1 = run == 0 ? (double)g : sums[0][c] + (double)g;
+        const double b1 = run == 0 ? (double)b : sums[1][c] + (double)b;
+        if (i0 < rows) {
+          sums[0][c] = g1;
+          sums[1][c] = b1;
+        } else {
+          pg[c] = (float)g1;
+          pg[cols + c] = (float)b1;
+        }
       }
-      pg[c] = g;
-      pg[cols + c] = b;
     }
   }
 }
 
 // Sums of the blocks' partial sums, fp64: a block takes 16 of the 2 cols sums, and
 // each of 64 groups of 4 lanes every 64th partial of them, then the groups' sums by
-// a fixed tree.  Its 256-1536 parts are 0.1-5 MB, and the chain of dependent loads is its
-// time: 4-5 us, 14-25 with 8 groups of 32 lanes.
+// a fixed tree.  Of 256-1536 parts a group adds 4-24, and the chain of dependent loads is
+// its time: 4-5 us at up to 1433 columns, 14-25 with 8 groups of 32 lanes.  (Rows that
+// take a block leave a part every 64 of them.)
 __global__ __launch_bounds__(kB) void k_norm_sum(int32_t cols, int64_t chunks,
                                                  const float* __restrict__ part,
                                                  float* __restrict__ dgamma,
