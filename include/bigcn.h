@@ -397,7 +397,9 @@ bigcn_status bigcn_restore_q8(const int8_t* codes, int64_t ldc, const float* qsc
  *           scales fp32[rows], as bigcn_binarize_pack writes them for the fp32 y
  *           (before a rounding to xtype), with rowptr and norm as there; pad bits
  *           and pad words are written as zero.
- * A row that holds a NaN or an infinity is NaN in y; other rows are not affected.
+ * A row that holds a NaN or an infinity is NaN in y; other rows are not affected.  Rows
+ * of finite elements of any size are normalised (where sums or squares pass fp32's
+ * range they are formed from the row times 2^-80).
  * Errors: EINVAL (rows < 0, cols < 1, short leading dimensions, bad type or norm,
  *         eps not finite or below the smallest normal fp32, NULL x with rows > 0,
  *         no output, one of a pair without the other), EALIGN, EUNSUPPORTED
@@ -423,7 +425,9 @@ bigcn_status bigcn_layernorm(const void* x, bigcn_dtype xtype, int64_t rows, int
  *           where x is not positive (exact from a checkpoint too).
  * Outputs, each NULL if not wanted, at least one given:
  *   dx      [rows][lddx] of type dtype; may be dy itself (with lddx = lddy), else
- *           it overlaps no other argument.
+ *           it overlaps no other argument.  From a checkpoint xhat is that of the
+ *           restored row: where a row's deviation is below its steps, so is what
+ *           xhat means, and |x| rstd has to be finite.
  *   dgamma, dbeta  fp32[cols]; with rows == 0 they are set to zero.
  *   workspace  bigcn_layernorm_backward_workspace_bytes(rows, cols) bytes, 256-byte
  *           aligned, contents on entry ignored; needed for dgamma or dbeta only.  At most

@@ -123,29 +123,59 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm(
       if (in && l16 < NV && group16 < groups) o.qscale[i * o.ldq + group16] = step;
     }
     if constexpr (!NORM) continue;
-    float s = 0.f;
+    // v less its mean, which is left in mean; returns the sum of its squares
+    float mean;
+    auto centre = [&] {
+      float s = 0.f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) s += (v[k][0] + v[k][1]) + (v[k][2] + v[k][3]);
-    // (the quotient corrected by its remainder: the mean of equal elements is that
-    // element)
-    s = row_sum<W, L>(s, slots[0]);
-    float mean = s * inv_cols;
-    mean = __builtin_fmaf(__builtin_fmaf(-mean, (float)cols, s), inv_cols, mean);
-    float s2 = 0.f;
+      for (int k = 0; k < NV; ++k) s += (v[k][0] + v[k][1]) + (v[k][2] + v[k][3]);
+      // (the quotient corrected by its remainder: the mean of equal elements is that
+      // element)
+      s = row_sum<W, L>(s, slots[0]);
+      mean = s * inv_cols;
+      mean = __builtin_fmaf(__builtin_fmaf(-mean, (float)cols, s), inv_cols, mean);
+      float s2 = 0.f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      v[k] -= mean;
-      const f32x4 c = m.owned(k, v[k]);
-      s2 += (c[0] * c[0] + c[1] * c[1]) + (c[2] * c[2] + c[3] * c[3]);
+      for (int k = 0; k < NV; ++k) {
+        v[k] -= mean;
+        const f32x4 c = m.owned(k, v[k]);
+        s2 += (c[0] * c[0] + c[1] * c[1]) + (c[2] * c[2] + c[3] * c[3]);
+      }
+      return row_sum<W, L>(s2, slots[1]);
+    };
+    float rstd = rsqrt1(centre() * inv_cols + eps), rstd_v = rstd;  // (of x and of v)
+    // Finite elements whose sum or squares pass fp32's range (from about 1e17 on; rows that
+    // hold an infinity or a NaN come here too): once more with the row read again times
+    // 2^-80, whose largest is 2^-23 to 2^48 then.  Rows beside them get the same again.
+    if constexpr (!std::is_same<T, F16>::value) {
+      const bool over = !(rstd > 0.f);  // (0 * infinity of an infinite variance is NaN)
+      if (__builtin_amdgcn_ballot_w64(over) != 0) {
+        const float down = over ? 0x1p-80f : 1.f, up = over ? 0x1p80f : 1.f;
+        int64_t j = i;  // (its addresses anew: the first ones held until here cost registers)
+        if constexpr (W > 1)
+          asm volatile("" : "+s"(j));
+        else
+          asm volatile("" : "+v"(j));
+        fetch(j, raw);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) v[k] = m.owned(k, to_f32(raw[k])) * down;
+        const float var = centre() * inv_cols, whole = var * up * up + eps;
+        mean *= up;
+        // (finite where only sums passed the range; the limit: of a row of equal elements,
+        // whose v is zero)
+        const bool back = whole < INFINITY;
+        const float r = over ? rsqrt1(back ? whole : var + eps * down * down) : rstd;
+        rstd = back ? r : r * down;
+        rstd_v = back ? fminf(r * up, FLT_MAX) : r;
+      }
     }
-    const float rstd = rsqrt1(row_sum<W, L>(s2, slots[1]) * inv_cols + eps);
-    f32x4 y[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) y[k] = ga[k] * (v[k] * rstd) + be[k];
     if (in && m.t == 0) {
       if (o.mean != nullptr) o.mean[i] = mean;
       if (o.rstd != nullptr) o.rstd[i] = rstd;
     }
+    f32x4 y[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) y[k] = ga[k] * (v[k] * rstd_v) + be[k];
     if (o.bits != nullptr) {
       float l1 = 0.f;
       uint32_t lo = 0, hi = 0;
@@ -283,10 +313,12 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm_grad(
           for (int u = 0; u < 4; ++u) neg |= c[u] > 0.f ? 0u : 1u << (4 * k + u);
       }
     } else {
+      // (halves: x - mean may be past fp32's range, its half is not)
+      const float half_mean = 0.5f * r.mean, twice_rstd = 2.f * r.rstd;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const f32x4 x = to_f32(r.x[k]);
-        xh[k] = (x - r.mean) * r.rstd;
+        xh[k] = (x * 0.5f - half_mean) * twice_rstd;
         if (relu)
 #pragma unroll
           for (int u = 0; u < 4; ++u) neg |= x[u] > 0.f ? 0u : 1u << (4 * k + u);
