@@ -183,14 +183,11 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm(
       for (int k = 0; k < NV; ++k) {
         const f32x4 ay = m.owned(k, y[k]);
         l1 += (fabsf(ay[0]) + fabsf(ay[1])) + (fabsf(ay[2]) + fabsf(ay[3]));
-        // the sign bits, element 3 first (-0 made +0: y >= 0 packs as a set bit)
+        // the sign bits, element 3 first: a bit is set for y >= 0 (-0 too, a NaN not)
         uint32_t nib = 0;
 #pragma unroll
-        for (int u = 3; u >= 0; --u) {
-          const float z = y[k][u] + 0.f;
-          nib = __builtin_amdgcn_alignbit(nib, __builtin_bit_cast(uint32_t, z), 31);
-        }
-        nib = ~nib & (k + 1 < NV ? 15u : owned_bits);
+        for (int u = 3; u >= 0; --u) nib = nib + nib + (y[k][u] >= 0.f ? 1u : 0u);
+        if (k + 1 == NV) nib &= owned_bits;
         if (k + 1 == NV) nib >>= m.skip;
         uint32_t w = nib << (4 * (m.t & 7));
         w |= dpp_u32<kXor1>(w);

@@ -1,4 +1,5 @@
-"""Layer norm at the ends of its types' range: finite rows whose sums or squares pass it."""
+"""Layer norm at the ends of its types' range: finite rows whose sums or squares pass it,
+and the signs of what is no number."""
 import numpy as np
 import pytest
 import torch
@@ -114,3 +115,28 @@ def test_gradients_of_finite_rows(cols, dtype, source):
     ro.within(ro.f64(dx), ref["dx"], ref["ddx"] + ro.store_bound(np.abs(ref["dx"]) + ref["ddx"], dtype), "dx")
     ro.within(ro.f64(dg), ref["dgamma"], ref["ddgamma"], "dgamma")
     ro.within(ro.f64(db), ref["dbeta"], ref["ddbeta"], "dbeta")
+
+
+@pytest.mark.parametrize("cols", [1, 3, 64, 100, 300, 602, 1433, 2049, 5000])
+def test_bits_of_what_is_no_number(cols):
+    """The packed signs are those of the pack of the fp32 y, which sets no bit for a NaN and
+    sets the bit of -0."""
+    rng = np.random.default_rng(cols)
+    x = torch.from_numpy(rng.standard_normal((24, cols)).astype(np.float32)).cuda()
+    nan = np.array([0x7FC00000, 0xFFC00000], np.uint32).view(np.float32)     # of either sign
+    x[3, 0], x[4, cols - 1] = float(nan[0]), float("inf")
+    x[5].view(torch.int32)[cols // 2] = -0x400000
+    x[6] = float("-inf")
+    assert int(torch.isnan(x).sum()) == 2
+    gamma = torch.from_numpy(rng.uniform(-1.5, 1.5, cols).astype(np.float32)).cuda()
+    beta = torch.from_numpy(rng.uniform(-0.5, 0.5, cols).astype(np.float32)).cuda()
+    gamma[cols // 3], beta[cols // 3] = 0.0, -0.0
+    for bad in (False, True):
+        if bad:
+            gamma[cols // 2] = float("nan")
+        got = every_output(x, gamma, beta)
+        bits, scale = torch.empty_like(got["bits"]), torch.empty_like(got["scale"])
+        bg.bigcn_binarize_pack(got["y"], bits, scale)
+        assert torch.equal(bits, got["bits"])
+        assert int(got["bits"][3:7].abs().sum()) == 0
+        assert torch.equal(torch.isnan(scale), torch.isnan(got["scale"]))
