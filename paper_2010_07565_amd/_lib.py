@@ -369,8 +369,14 @@ def bigcn_layer_backward_packed(rowptr: torch.Tensor, colidx: torch.Tensor,
     n = rowptr.shape[0] - 1
     d_out, d_in = wt.shape
     nnz = colidx.shape[0] if nnz is None else nnz
+    _len(rowptr, "rowptr", n + 1)
+    _len(colidx, "colidx", nnz)
+    _len(slot, "slot", n)
+    _len(colslot, "colslot", nnz)
     _rows(hbits, "hbits", n, words(d_in))
     _len(hscale, "hscale", n)
+    _rows(wbits, "wbits", d_out, words(d_in))
+    _len(alpha, "alpha", d_out)
     _rows(gout, "gout", n, d_out)
     _rows(dh, "dh", n, d_in)
     _rows(dh_tilde, "dh_tilde", n, d_in)

@@ -1,5 +1,8 @@
 """The training operators' workspace sizes at their largest, and the binding's checks.
 No GPU is needed."""
+import pytest
+import torch
+
 import paper_2010_07565_amd as bg
 
 
@@ -18,3 +21,38 @@ def test_workspace_of_the_norm_gradients():
             assert 0 < bg.layernorm_backward_workspace_bytes(rows, cols) <= sets * 2 * cols * 4 + 256
     assert bg.layernorm_backward_workspace_bytes(0, 64) == 0
     assert bg.layernorm_backward_workspace_bytes(most + 1, 8192) == 0    # (refused)
+
+
+N, NNZ, D_IN, D_OUT = 50, 200, 100, 16
+
+
+def packed_arguments():
+    return dict(rowptr=torch.zeros(N + 1, dtype=torch.int64),
+                colidx=torch.zeros(NNZ, dtype=torch.int32),
+                hbits=torch.zeros(N, 2, dtype=torch.int64), hscale=torch.zeros(N),
+                wt=torch.zeros(D_OUT, D_IN), wbits=torch.zeros(D_OUT, 2, dtype=torch.int64),
+                alpha=torch.zeros(D_OUT), gout=torch.zeros(N, D_OUT), dwt=torch.zeros(D_OUT, D_IN),
+                workspace=torch.zeros(1 << 20, dtype=torch.uint8),
+                slot=torch.zeros(N, dtype=torch.int32), colslot=torch.zeros(NNZ, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("name,short", [
+    ("wbits", torch.zeros(D_OUT - 1, 2, dtype=torch.int64)),
+    ("wbits", torch.zeros(D_OUT, 1, dtype=torch.int64)),
+    ("alpha", torch.zeros(D_OUT - 1)), ("alpha", torch.zeros(2 * D_OUT)[::2]),
+    ("alpha", torch.zeros(1, D_OUT)),
+    ("slot", torch.zeros(N - 1, dtype=torch.int32)),
+    ("colslot", torch.zeros(NNZ - 1, dtype=torch.int32)),
+    ("colidx", torch.zeros(2 * NNZ, dtype=torch.int32)[::2]),
+    ("rowptr", torch.zeros(2 * N + 2, dtype=torch.int64)[::2]),
+    ("hbits", torch.zeros(N, 1, dtype=torch.int64)), ("hscale", torch.zeros(N - 1)),
+    ("nnz", NNZ + 1)])
+def test_packed_backward_refuses_short_arguments(name, short):
+    """By name, before anything is asked of the device."""
+    args = packed_arguments()
+    with pytest.raises(ValueError, match="rowptr must be a device tensor"):
+        bg.bigcn_layer_backward_packed(**args)         # all of them right, and on the host
+    args[name] = short
+    with pytest.raises(ValueError, match="colidx" if name == "nnz" else name) as e:
+        bg.bigcn_layer_backward_packed(**args)
+    assert "device tensor" not in str(e.value)
