@@ -166,3 +166,23 @@ def test_forward_over_several_turns(cols, rows, dtype):
     on = (bits[:, at // 64] >> (at % 64)) & 1
     sure = ref.abs() > lim
     assert bool(((on == 1) == (ref >= 0))[sure].all())
+
+
+def test_the_current_stream_is_the_calls():
+    """Without a stream a call is on the current one: in order with what is enqueued there."""
+    import paper_2010_07565_amd._lib as lib
+    side = torch.cuda.Stream()
+    assert lib._stream(None) == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(side):
+        assert lib._stream(None) == side.cuda_stream == torch.cuda.current_stream().cuda_stream
+    x = torch.empty(300001, 256, device="cuda")
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for k in range(3):
+            x.normal_()
+            bg.bigcn_layernorm(x, eps=ro.EPS, y=y)
+        z.copy_(y)
+    side.synchronize()
+    bg.bigcn_layernorm(x, eps=ro.EPS, y=y)
+    assert torch.equal(y, z)

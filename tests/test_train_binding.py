@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2010_07565_amd as bg
+from paper_2010_07565_amd import _lib
 
 
 def test_workspace_of_the_norm_gradients():
@@ -56,3 +57,20 @@ def test_packed_backward_refuses_short_arguments(name, short):
     with pytest.raises(ValueError, match="colidx" if name == "nnz" else name) as e:
         bg.bigcn_layer_backward_packed(**args)
     assert "device tensor" not in str(e.value)
+
+
+def test_current_stream_without_the_private_functions(monkeypatch):
+    """Calls without a stream take torch's current one by its public interface where a torch
+    has no other."""
+    class Stream:
+        cuda_stream = 77
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Stream())
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        with monkeypatch.context() as m:
+            m.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+            m.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 55)
+            assert _lib._stream(None) == 55
+            m.delattr(torch._C, name)
+            assert _lib._stream(None) == 77
+    assert _lib._stream(Stream()) == 77 and _lib._stream(9) == 9
