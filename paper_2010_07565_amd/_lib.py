@@ -427,6 +427,15 @@ def _dtype(t: torch.Tensor, name: str) -> int:
     return DTYPES[t.dtype]
 
 
+def _sizes(t: torch.Tensor, name: str):
+    """Rows and columns of a call's matrix; columns are 32-bit numbers there."""
+    shape = t.shape
+    if len(shape) != 2 or shape[1] > 0x7FFFFFFF:
+        raise ValueError("%s must be a matrix of less than 2^31 columns, got %s"
+                         % (name, tuple(shape)))
+    return shape
+
+
 def _mat(t: Optional[torch.Tensor], dtype, name: str, rows: int, cols: int):
     """Pointer and leading dimension of an optional matrix argument.  (A call has
     up to ten: what is right is told with few lookups, the rest says what is not.)"""
@@ -466,8 +475,8 @@ def bigcn_checkpoint_q8(x: torch.Tensor, codes: torch.Tensor, qscale: torch.Tens
     [rows, cols] and fp32 scales [rows, checkpoint_groups(cols)]; signs and zeros
     are kept exactly (see include/bigcn.h)."""
     xt = _dtype(x, "x")
+    rows, cols = _sizes(x, "x")
     px, ldx = _mat(x, x.dtype, "x", 0, 0)
-    rows, cols = x.shape
     st = load().bigcn_checkpoint_q8(
         px, xt, rows, cols, ldx, *_mat(codes, torch.int8, "codes", rows, cols),
         *_mat(qscale, torch.float32, "qscale", rows, checkpoint_groups(cols)), _stream(stream))
@@ -478,8 +487,8 @@ def bigcn_restore_q8(codes: torch.Tensor, qscale: torch.Tensor, y: torch.Tensor,
                      stream=None) -> None:
     """Writes a checkpoint's activations, rounded to y's type, into y [rows, cols]."""
     yt = _dtype(y, "y")
+    rows, cols = _sizes(y, "y")
     py, ldy = _mat(y, y.dtype, "y", 0, 0)
-    rows, cols = y.shape
     st = load().bigcn_restore_q8(
         *_mat(codes, torch.int8, "codes", rows, cols),
         *_mat(qscale, torch.float32, "qscale", rows, checkpoint_groups(cols)),
@@ -495,8 +504,8 @@ def bigcn_layernorm(x: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, y
     packed signs and row scales of y (bits, scale; rowptr and norm as for
     bigcn_binarize_pack)."""
     xt = _dtype(x, "x")
+    rows, cols = _sizes(x, "x")
     px, ldx = _mat(x, x.dtype, "x", 0, 0)
-    rows, cols = x.shape
     f = torch.float32
     py, ldy = _mat(y, x.dtype, "y", rows, cols)
     pc, ldc = _mat(codes, torch.int8, "codes", rows, cols)
@@ -522,8 +531,8 @@ def bigcn_layernorm_backward(dy: torch.Tensor, mean: torch.Tensor, rstd: torch.T
     a ReLU's output and dx the gradient before it.  workspace
     (layernorm_backward_workspace_bytes) is needed for dgamma and dbeta."""
     dt = _dtype(dy, "dy")
+    rows, cols = _sizes(dy, "dy")
     py, lddy = _mat(dy, dy.dtype, "dy", 0, 0)
-    rows, cols = dy.shape
     f = torch.float32
     px, ldx = _mat(x, dy.dtype, "x", rows, cols)
     pc, ldc = _mat(codes, torch.int8, "codes", rows, cols)
@@ -551,8 +560,8 @@ def bigcn_softmax_xent(logits: torch.Tensor, labels: torch.Tensor, weight: float
     [0, classes) for a row without one.  workspace (softmax_xent_workspace_bytes)
     is needed for loss."""
     dt = _dtype(logits, "logits")
+    rows, cols = _sizes(logits, "logits")
     pz, ldz = _mat(logits, logits.dtype, "logits", 0, 0)
-    rows, cols = logits.shape
     pd, lddz = _mat(dlogits, logits.dtype, "dlogits", rows, cols)
     st = load().bigcn_softmax_xent(
         pz, dt, rows, cols, ldz, _vec(labels, torch.int32, "labels", rows), weight,

@@ -74,3 +74,14 @@ def test_current_stream_without_the_private_functions(monkeypatch):
             m.delattr(torch._C, name)
             assert _lib._stream(None) == 77
     assert _lib._stream(Stream()) == 77 and _lib._stream(9) == 9
+
+
+def test_more_columns_than_32_bits_count():
+    """Refused: the columns' low 32 bits (70 here) are not what was asked for."""
+    x = torch.zeros(1, 1).expand(1, (1 << 32) + 70)
+    v = torch.zeros(1)
+    for call in (lambda: bg.bigcn_checkpoint_q8(x, None, None), lambda: bg.bigcn_restore_q8(None, None, x),
+                 lambda: bg.bigcn_layernorm(x, y=x), lambda: bg.bigcn_layernorm_backward(x, v, v, x=x, dx=x),
+                 lambda: bg.bigcn_softmax_xent(x, v.int(), loss=v)):
+        with pytest.raises(ValueError, match="columns"):
+            call()
