@@ -1098,6 +1098,12 @@ bigcn_status layer_backward(int64_t n, int64_t nnz, const int64_t* rowptr,
                                    L.kw, beta, s));
   const uint64_t* Fs = kept ? in.hbits : F;
   const int64_t ldfs = kept ? in.ldhb : L.kw;
+  auto copy_dzeta = [&] {
+    return n == 0 || dzeta == nullptr || z_direct
+               ? hipSuccess
+               : hipMemcpy2DAsync(dzeta, lddz * 4, dz, L.ldm * 4, (size_t)d_out * 4, n,
+                                  hipMemcpyDeviceToDevice, s);
+  };
   prep(Gm, in.hscale);
   BIGCN_CHECK(hipGetLastError());
   if (db != nullptr) {
@@ -1117,9 +1123,7 @@ bigcn_status layer_backward(int64_t n, int64_t nnz, const int64_t* rowptr,
                                    mean ? 2 : 0, sc, Gsrc,
                                    bigcn::IType::F32, d_out, ldsrc, ones, nullptr, 0, dz,
                                    ldz, plan, wsp, s));
-    if (dzeta != nullptr && !z_direct)
-      BIGCN_CHECK(hipMemcpy2DAsync(dzeta, lddz * 4, dz, L.ldm * 4, (size_t)d_out * 4, n,
-                                   hipMemcpyDeviceToDevice, s));
+    if (!kept) BIGCN_CHECK(copy_dzeta());
   }
   // dW~^T, then Eq. (15).
   switch (L.ntw) {
@@ -1128,6 +1132,7 @@ bigcn_status layer_backward(int64_t n, int64_t nnz, const int64_t* rowptr,
     case 4: launch_wtilde<4>(n, d_in, d_out, L, Fs, ldfs, beta, dz, ldz, pw, s); break;
     default: launch_wtilde<8>(n, d_in, d_out, L, Fs, ldfs, beta, dz, ldz, pw, s); break;
   }
+  if (kept) BIGCN_CHECK(copy_dzeta());  // (dzeta may lie over the signs, read until here)
   launch_chunk_sums(db_sum, dw_sum(), s);
   hipLaunchKernelGGL(k_bwd_weights, dim3((unsigned)d_out), dim3(kB), 0, s, d_in, wtd, wbits,
                      ldw, alpha, wt, ldwt, dwt, lddw);
