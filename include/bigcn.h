@@ -399,7 +399,9 @@ bigcn_status bigcn_restore_q8(const int8_t* codes, int64_t ldc, const float* qsc
  *           and pad words are written as zero.
  * A row that holds a NaN or an infinity is NaN in y; other rows are not affected.  Rows
  * of finite elements of any size are normalised (where sums or squares pass fp32's
- * range they are formed from the row times 2^-80).
+ * range they are formed from the row times 2^-80).  Sums over a row are formed in fp32
+ * by a tree over chains of at most 40 additions; 1 / sqrt is the hardware's estimate and
+ * one Newton step, within 1.5 units in the last place.
  * Errors: EINVAL (rows < 0, cols < 1, short leading dimensions, bad type or norm,
  *         eps not finite or below the smallest normal fp32, NULL x with rows > 0,
  *         no output, one of a pair without the other), EALIGN, EUNSUPPORTED
@@ -466,6 +468,10 @@ bigcn_status bigcn_layernorm_backward(const void* dy, bigcn_dtype dtype, int64_t
  * probability zero and gradient zero; a labelled row of nothing but -infinity
  * has no distribution: its loss is +infinity and its gradient zero.  The sum
  * over rows is formed in fp64 in a fixed order: reproducible bit for bit.
+ * The exponentials and the logarithm are the hardware's, in fp32: with M the row's
+ * maximum a probability is within (8 (M - z_ik) + 64) 2^-24 of itself, and that much of
+ * the sum's other terms (it may be zero below 2^-126); a row's loss is within what
+ * that makes of the sum's logarithm and 2^-22 (|M| + |log sum| + |z_i,label_i|).
  * Errors: EINVAL (rows < 0, cols < 1, short leading dimensions, bad type, weight
  *         not finite, NULL logits or labels with rows > 0, no output), EALIGN,
  *         EWORKSPACE, EUNSUPPORTED (cols > 8192).
