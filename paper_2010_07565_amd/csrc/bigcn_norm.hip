@@ -433,6 +433,11 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kW)) void k_norm_grad(
           g += red[w][c + back];
           b += red[kW + w][c + back];
         }
+        if (run == 0 && i0 >= rows) {  // the only run
+          pg[c] = g;
+          pg[cols + c] = b;
+          continue;
+        }
         const double g1 = run == 0 ? (double)g : sums[0][c] + (double)g;
         const double b1 = run == 0 ? (double)b : sums[1][c] + (double)b;
         if (i0 < rows) {
