@@ -60,7 +60,7 @@ struct NormOut {
 // The forward: the mean, then the mean square of the centred values (a second pass over
 // the registers: nothing cancels), y, and from y what the caller asked for.
 // 2449029 x 256 fp32: to y 873 us (5.7 TB/s), to signs, scales and checkpoint 629 (5.3);
-// 232965 x 602 bf16: 110 (5.1) and 127 (3.6, by then bound by its instructions).
+// 232965 x 602 bf16: 110 (5.1) and 130 (3.5, by then bound by its instructions).
 // Every row is read once and stays in registers; L lanes hold it (or W
 // waves, one row a block), 64 / L rows a wave.  (Issuing the next rows' loads before
 // this row's arithmetic measured no faster: other waves' loads fill the time.)
@@ -233,7 +233,7 @@ struct Kept {
 
 // The backward: the row's two sums, dx and the terms of dgamma and dbeta in one pass over
 // dy and x, or over dy and the 1.06 bytes an element of x's checkpoint.  2449029 x 256
-// fp32: 1380 us from x (5.5 TB/s), 1020-1100 from the checkpoint (5.2-5.6); 169343 x 128
+// fp32: 1380 us from x (5.5 TB/s), 1020-1120 from the checkpoint (5.1-5.6); 169343 x 128
 // fp32: 45-49 and 37; 232965 x 602 bf16: 158 and 135 (5.3).
 // Each row is held in registers as in the forward, blocks taking rows in
 // turn; dx is written, and each lane adds its columns' terms of dgamma and dbeta over
